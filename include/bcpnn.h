@@ -30,8 +30,8 @@
  * destroy).  Caller buffers named *_dev are device pointers (16-byte aligned, contiguous) that
  * the caller owns; *_host are host pointers.  Every call enqueues its kernels on the stream
  * given to create and returns without waiting, except get_state, set_state, get_mi, the
- * profile reads and structural_update with a non-NULL count pointer, which wait for the
- * stream.  Calls on one layer must not run concurrently from several host threads.
+ * profile reads, structural_update with a non-NULL count pointer and mx_from_layer, which wait
+ * for the stream.  Calls on one layer must not run concurrently from several host threads.
  *
  * Second stream: train_batch updates, on the caller's stream, everything the next batch reads
  * (Pij and w of active blocks, Pi, Pj, b, the activities).  The Pij of silent blocks are
@@ -330,7 +330,8 @@ typedef struct bcpnn_mx bcpnn_mx;
 bcpnn_status bcpnn_mx_create(const bcpnn_config *cfg, const uint8_t *mask_host, const float *w_dev,
                              const float *b_dev, void *hip_stream, bcpnn_mx **out);
 
-/* From a layer's present weights, biases and mask, on the layer's stream.  Waits for it. */
+/* From a layer's present weights, biases and mask, on the layer's stream.  Waits for it, so it reports
+ * what train_batch saw of its inputs (EINPUT).  Errors: EINVAL, ENOMEM, EDEVICE, ESTATE, EINPUT. */
 bcpnn_status bcpnn_mx_from_layer(bcpnn_layer *layer, bcpnn_mx **out);
 
 /* Releases the 4-bit layer after its stream is idle.  NULL is ignored. */

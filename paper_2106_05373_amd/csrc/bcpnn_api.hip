@@ -780,6 +780,9 @@ bcpnn_status bcpnn_mx_from_layer(bcpnn_layer* L, bcpnn_mx** out) {
     if (!out) return fail(BCPNN_EINVAL, "out is NULL");
     *out = nullptr;
     if (bcpnn_status st = usable(L)) return st;
+    HIP_TRY(L, read_input_check(L));
+    HIP_TRY(L, hipStreamSynchronize(L->stream));
+    if (bcpnn_status st = input_check_result(L)) return st;
     return bcpnn::mx_layer_make(L->cfg, L->w, L->b,
                                 bcpnn::ActiveLists{L->act_list, L->act_count, L->cfg.in_hcu, L->max_active},
                                 L->stream, out);
