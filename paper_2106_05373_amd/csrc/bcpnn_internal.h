@@ -277,7 +277,6 @@ hipError_t launch_mx_forward(hipStream_t stream, const Geometry& g, const float*
                              int64_t turned_rows, float* y, float* s, int32_t* winner);
 int64_t mx_forward_turned_rows(const Geometry& g, int32_t max_batch);
 hipError_t mx_forward_prepare();     // before the first launch on a device
-int32_t mx_forward_most_rows(const Geometry& g);   // rows that one launch can take
 
 // Makes a 4-bit layer from device arrays w [n_in][n_out], b and lists, on `stream`.  Waits.
 bcpnn_status mx_layer_make(const bcpnn_config& cfg, const float* w, const float* b, const ActiveLists& act,

@@ -418,20 +418,18 @@ hipError_t mx_forward_prepare() {
     return e;
 }
 
-int32_t mx_forward_most_rows(const Geometry& g) {
-    const int64_t wgs = ((1ll << 32) - 1) / (64 * kMxWaves);   // below 2^32 work-items
-    return (int32_t)std::min<int64_t>(wgs / g.out_hcu * kMxRows, 1 << 30);
-}
-
 // Rows of the transposed input: as many as a batch has, within 64 MiB.
 int64_t mx_forward_turned_rows(const Geometry& g, int32_t max_batch) {
     const int64_t fit = (64ll << 20) / 4 / g.n_in / 64 * 64;
     return std::min<int64_t>(fit, ((int64_t)max_batch + 63) / 64 * 64);
 }
 
-hipError_t launch_mx_forward(hipStream_t stream, const Geometry& g, const float* x, int32_t B, const void* codes,
-                             const void* scales, const float* bias, const ActiveUnits& act, float gain, float* turned,
-                             int64_t turned_rows, float* y, float* s, int32_t* winner) {
+namespace {
+
+// Rows that one launch of each kernel takes (mx_launch_rows).
+hipError_t forward_part(hipStream_t stream, const Geometry& g, const float* x, int32_t B, const void* codes,
+                        const void* scales, const float* bias, const ActiveUnits& act, float gain, float* turned,
+                        int64_t turned_rows, float* y, float* s, int32_t* winner) {
     const int vec = mx_gather_width(g.in_mcu);
     if (mx_rows_in_lds(g, B)) {
         auto* kernel = vec == 4   ? &forward_rows_kernel<4>
@@ -460,6 +458,21 @@ hipError_t launch_mx_forward(hipStream_t stream, const Geometry& g, const float*
             g, f, xr, (int32_t)turned_rows, n, (const uint8_t*)codes, (const uint32_t*)scales, bias, act, gain,
             y ? y + r * g.n_out : nullptr, s ? s + r * g.n_out : nullptr, winner ? winner + r * g.out_hcu : nullptr);
         const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_mx_forward(hipStream_t stream, const Geometry& g, const float* x, int32_t B, const void* codes,
+                             const void* scales, const float* bias, const ActiveUnits& act, float gain, float* turned,
+                             int64_t turned_rows, float* y, float* s, int32_t* winner) {
+    const int64_t most = mx_launch_rows(g);
+    for (int64_t r = 0; r < B; r += most) {
+        const hipError_t e = forward_part(stream, g, x + r * g.n_in, (int32_t)std::min<int64_t>(most, B - r), codes,
+                                          scales, bias, act, gain, turned, turned_rows, y ? y + r * g.n_out : nullptr,
+                                          s ? s + r * g.n_out : nullptr, winner ? winner + r * g.out_hcu : nullptr);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -85,9 +85,8 @@ bcpnn_status forward(bcpnn_mx* m, const float* x, int32_t B, float* y, float* s,
 }
 
 bcpnn_status check_batch(const bcpnn_mx* m, int32_t B) {
-    if (B < 1 || B > m->cfg.max_batch || B > bcpnn::mx_forward_most_rows(m->g))
-        return fail(BCPNN_EINVAL, "batch %d outside [1, %d]", B,
-                    std::min(m->cfg.max_batch, bcpnn::mx_forward_most_rows(m->g)));
+    if (B < 1 || B > m->cfg.max_batch)
+        return fail(BCPNN_EINVAL, "batch %d outside [1, %d]", B, m->cfg.max_batch);
     return BCPNN_OK;
 }
 
@@ -254,8 +253,7 @@ bcpnn_status bcpnn_mx_predict(bcpnn_mx* hidden, bcpnn_mx* readout, const float* 
     if (B < 1 || rows < 1) return fail(BCPNN_EINVAL, "B and rows must be positive");
     // rows per launch: whole row blocks, or as few as keep x 16-byte aligned
     const int64_t n_in = hidden->g.n_in;
-    int64_t step = std::min<int64_t>({rows, B, bcpnn::mx_forward_most_rows(hidden->g),
-                                      bcpnn::mx_forward_most_rows(readout->g)});
+    int64_t step = std::min(rows, B);
     if (step < B) {
         const int64_t unit = step >= 32 ? 32 : n_in % 4 == 0 ? 1 : n_in % 2 == 0 ? 2 : 4;
         step = step / unit * unit;

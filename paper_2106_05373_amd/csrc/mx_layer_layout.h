@@ -51,6 +51,13 @@ inline ForwardShape mx_forward_shape(const Geometry& g, int64_t kg, int64_t rows
     return f;
 }
 
+// Rows that a launch takes, whole row blocks: it stays below 2^32 work-items.  (A launch of so many
+// workgroups has the least waves for its column tiles; N_out <= 2^22 leaves room for two row blocks at least.)
+inline int64_t mx_launch_rows(const Geometry& g) {
+    const int64_t tiles = mx_row_blocks(g.out_mcu), waves = tiles <= 4 ? 4 : tiles <= 16 ? 8 : kMxWaves;
+    return ((1ll << 32) - 1) / (64 * waves) / g.out_hcu * kMxRows;
+}
+
 // The form for many rows of a narrow layer (forward_rows_kernel): 16 rows of the inputs in LDS.
 constexpr int kMxTileRows = 16;
 constexpr int kMxRowsLds = 150 * 1024;

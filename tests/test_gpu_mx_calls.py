@@ -40,3 +40,26 @@ def test_a_layer_whose_inputs_broke_their_pairs_is_not_copied():
             _mx().Layer.of(layer)
         with pytest.raises(B.BcpnnError, match="ESTATE"):
             _mx().Layer.of(layer)
+
+
+def test_every_batch_of_a_layer_of_very_many_hidden_hcus():
+    """2^21 hidden HCUs, the most for which 64 rows are a batch."""
+    import torch
+    B = _bcpnn()
+    ho, n = 1 << 21, 64
+    cfg = B.default_config(2, 1, ho, 1, n)
+    w = torch.randn(2, ho, generator=_gen(1), device="cuda")
+    b = torch.randn(ho, generator=_gen(2), device="cuda")
+    x = torch.rand(n, 2, generator=_gen(3), device="cuda")
+    with _mx().Layer(cfg, None, w, b) as layer:
+        y, s = (torch.full((n + 1, ho), 5.0, device="cuda") for _ in range(2))
+        for rows in (1, 33, n):
+            layer.forward(x[:rows], y[:rows], s[:rows])
+            xq = torch.from_numpy(mx_plain.quantized(x[:rows].cpu().numpy())).cuda()
+            wq = _mx().dequantize(_mx().quantize(w, rows=False, columns=True)).double().t()
+            want = xq @ wq + b.double()
+            mag = xq.abs() @ wq.abs() + b.double().abs()
+            assert bool(((s[:rows].double() - want).abs() <= mag * mx_plain.sum_bound(2)).all()), rows
+            assert bool((y[:rows] == 1.0).all()) and bool((y[rows:] == 5.0).all()) and bool((s[rows:] == 5.0).all())
+            y.fill_(5.0)
+            s.fill_(5.0)
