@@ -251,14 +251,10 @@ bcpnn_status bcpnn_mx_predict(bcpnn_mx* hidden, bcpnn_mx* readout, const float* 
     if (readout->g.n_in != hidden->g.n_out || readout->g.out_hcu != 1 || readout->stream != hidden->stream)
         return fail(BCPNN_EINVAL, "the readout must have one HCU over the hidden units, on one stream");
     if (B < 1 || rows < 1) return fail(BCPNN_EINVAL, "B and rows must be positive");
-    // rows per launch: whole row blocks, or as few as keep x 16-byte aligned
+    // Rows at a time: whole row blocks where there are so many.  (Any row of an aligned x will do as the first:
+    // it is read as many values at a time as divide a row.)
     const int64_t n_in = hidden->g.n_in;
-    int64_t step = std::min(rows, B);
-    if (step < B) {
-        const int64_t unit = step >= 32 ? 32 : n_in % 4 == 0 ? 1 : n_in % 2 == 0 ? 2 : 4;
-        step = step / unit * unit;
-        if (step == 0) return fail(BCPNN_EINVAL, "y_dev has too few rows for aligned inputs");
-    }
+    const int64_t step = rows >= B || rows < bcpnn::kMxRows ? rows : rows / bcpnn::kMxRows * bcpnn::kMxRows;
     for (int64_t k = 0; k < B; k += step) {
         const int32_t n = (int32_t)std::min<int64_t>(step, B - k);
         if (bcpnn_status st = forward(hidden, x_dev + k * n_in, n, y_dev, nullptr, nullptr)) return st;

@@ -63,3 +63,26 @@ def test_every_batch_of_a_layer_of_very_many_hidden_hcus():
             assert bool((y[:rows] == 1.0).all()) and bool((y[rows:] == 5.0).all()) and bool((s[rows:] == 5.0).all())
             y.fill_(5.0)
             s.fill_(5.0)
+
+
+@pytest.mark.parametrize("in_hcu,in_mcu", [(31, 1), (45, 2), (33, 3), (12, 4)])
+def test_predict_with_any_number_of_workspace_rows(in_hcu, in_mcu):
+    """Rows of x that start at any alignment of their elements."""
+    import torch
+    B, mx = _bcpnn(), _mx()
+    n_in = in_hcu * in_mcu
+    hidden = mx.Layer(B.default_config(in_hcu, in_mcu, 3, 9, 16), None,
+                      torch.randn(n_in, 27, generator=_gen(1), device="cuda"), torch.zeros(27, device="cuda"))
+    readout = mx.Layer(B.default_config(3, 9, 1, 6, 16), None,
+                       torch.randn(27, 6, generator=_gen(2), device="cuda"), torch.zeros(6, device="cuda"))
+    x = torch.rand(11, n_in, generator=_gen(3), device="cuda")
+    y = torch.empty(11, 27, device="cuda")
+    want = torch.empty(11, 1, device="cuda", dtype=torch.int32)
+    hidden.forward(x, y)
+    readout.readout(y, want)
+    for rows in (1, 2, 3, 5, 11):
+        got = torch.full((12,), -1, device="cuda", dtype=torch.int32)
+        hidden.predict_with(readout, x, torch.empty(rows, 27, device="cuda"), got[:11])
+        assert torch.equal(got[:11], want[:, 0]) and got[11] == -1, rows
+    hidden.close()
+    readout.close()
