@@ -116,19 +116,26 @@ class QuantizedNetwork:
 
     def predict(self, x, out=None):
         """Class index per sample ([B] int32, any B) of x [B][N_in] (CUDA float32, contiguous), as
-        Network.predict gives it.  Work of the current stream is waited for and made to wait."""
+        Network.predict gives it, into out of any type, if given (int32 and contiguous: directly, and
+        nothing is allocated).  Work of the current stream is waited for and made to wait."""
         torch = self.torch
+        B = x.shape[0]
+        win = out
+        if (out is None or not out.is_cuda or out.dtype != torch.int32 or out.shape != (B,)
+                or not out.is_contiguous()):
+            win = torch.empty(B, device="cuda", dtype=torch.int32)
+        if B > 0:
+            stream, current = self.hidden.stream, torch.cuda.current_stream()
+            other = stream.cuda_stream != current.cuda_stream
+            if other:
+                stream.wait_stream(current)
+            self.hidden.predict_with(self.readout, x, self._rows, win)
+            if other:
+                current.wait_stream(stream)
         if out is None:
-            out = torch.empty(x.shape[0], device="cuda", dtype=torch.int32)
-        if x.shape[0] == 0:
-            return out
-        stream, current = self.hidden.stream, torch.cuda.current_stream()
-        other = stream.cuda_stream != current.cuda_stream
-        if other:
-            stream.wait_stream(current)
-        self.hidden.predict_with(self.readout, x, self._rows, out)
-        if other:
-            current.wait_stream(stream)
+            return win
+        if out is not win:
+            out[:B].copy_(win)
         return out
 
     def close(self):

@@ -86,3 +86,35 @@ def test_predict_with_any_number_of_workspace_rows(in_hcu, in_mcu):
         assert torch.equal(got[:11], want[:, 0]) and got[11] == -1, rows
     hidden.close()
     readout.close()
+
+
+def _small_network():
+    import torch
+    from paper_2106_05373_amd.pipeline import Network
+    B = _bcpnn()
+    net = Network(B.default_config(64, 2, 4, 16, 32, alpha=0.05, seed=3), None, 5)
+    x = torch.rand(70, 128, generator=_gen(4), device="cuda")
+    target = torch.nn.functional.one_hot(torch.arange(32, device="cuda") % 5, 5).float()
+    for _ in range(4):
+        net.train_hidden(x[:32])
+        net.train_readout(x[:32], target)
+    return net, x
+
+
+def test_quantized_network_writes_every_output_that_a_network_writes():
+    import torch
+    net, x = _small_network()
+    q = net.quantized()
+    want = q.predict(x)
+    assert want.dtype == torch.int32 and want.shape == (70,)
+    room = torch.full((70, 3), -1, device="cuda", dtype=torch.int32)
+    outs = [torch.full((70,), -1, device="cuda", dtype=torch.int64), room[:, 1],
+            torch.full((70,), -1, dtype=torch.int32), torch.full((70,), -1.0, device="cuda")]
+    for out in outs:
+        assert net.predict(x, out=out) is out           # (the network itself takes them)
+        out.fill_(-1)
+        assert q.predict(x, out=out) is out
+        assert torch.equal(out.cuda().int(), want)
+    assert bool((room[:, 0] == -1).all()) and bool((room[:, 2] == -1).all())
+    q.close()
+    net.close()
