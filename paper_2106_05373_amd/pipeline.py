@@ -112,7 +112,9 @@ class QuantizedNetwork:
         self.readout = mx.Layer.of(net.readout)
         self.n_classes = net.n_classes
         rows = max(32, min(8192, (1 << 24) // self.hidden.n_out // 32 * 32))
-        self._rows = torch.empty((rows, self.hidden.n_out), device="cuda", dtype=torch.float32)
+        # (memory of the stream that uses it: no other stream's work on it can be pending)
+        with torch.cuda.stream(self.hidden.stream):
+            self._rows = torch.empty((rows, self.hidden.n_out), device="cuda", dtype=torch.float32)
 
     def predict(self, x, out=None):
         """Class index per sample ([B] int32, any B) of x [B][N_in] (CUDA float32, contiguous), as

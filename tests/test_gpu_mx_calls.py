@@ -118,3 +118,19 @@ def test_quantized_network_writes_every_output_that_a_network_writes():
     assert bool((room[:, 0] == -1).all()) and bool((room[:, 2] == -1).all())
     q.close()
     net.close()
+
+
+def test_quantized_network_holds_its_workspace_on_its_stream():
+    """Every prediction uses it there, whichever stream is current when it is made or called: memory of
+    another stream's pool may still be in use by work that this stream does not wait for."""
+    import torch
+    from paper_2106_05373_amd.pipeline import Network
+    B = _bcpnn()
+    own = torch.cuda.Stream()
+    net = Network(B.default_config(64, 2, 4, 16, 32), None, 5, stream=own)
+    q = net.quantized()
+    at = q._rows.data_ptr()
+    held = [s for s in torch.cuda.memory_snapshot() if s["address"] <= at < s["address"] + s["total_size"]]
+    assert len(held) == 1 and held[0]["stream"] == own.cuda_stream
+    q.close()
+    net.close()
