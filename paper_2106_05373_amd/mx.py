@@ -163,12 +163,16 @@ def product(a: Matrix, b: Matrix, bias: Optional[torch.Tensor] = None, alpha: fl
 
 class Layer:
     """A BCPNN layer for inference on 4-bit weights and inputs (one bcpnn_mx), from the dense weights
-    w [N_in][N_out] and biases b [N_out] on the GPU; `of` makes it from a trained bcpnn.Layer."""
+    w [N_in][N_out] and biases b [N_out] on the GPU (work of the current stream on them is waited for);
+    `of` makes it from a trained bcpnn.Layer."""
 
     def __init__(self, cfg: bcpnn.Config, mask: Optional[np.ndarray], w: torch.Tensor, b: torch.Tensor,
                  stream=None):
         n_in, n_out = cfg.in_hcu * cfg.in_mcu, cfg.out_hcu * cfg.out_mcu
-        stream = torch.cuda.current_stream() if stream is None else stream
+        current = torch.cuda.current_stream()
+        stream = current if stream is None else stream
+        if stream.cuda_stream != current.cuda_stream:
+            stream.wait_stream(current)
         keep = None if mask is None else _host(mask, np.uint8, (cfg.in_hcu, cfg.out_hcu))
         h = ctypes.c_void_p()
         _check(lib.bcpnn_mx_create(ctypes.byref(cfg), None if keep is None else keep.ctypes.data,

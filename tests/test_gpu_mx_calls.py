@@ -134,3 +134,29 @@ def test_quantized_network_holds_its_workspace_on_its_stream():
     assert len(held) == 1 and held[0]["stream"] == own.cuda_stream
     q.close()
     net.close()
+
+
+def test_a_layer_on_another_stream_waits_for_its_weights():
+    import torch
+    B = _bcpnn()
+    cfg = B.default_config(100, 2, 3, 40, 32)
+    final = torch.randn(200, 120, generator=_gen(1), device="cuda")
+    x = torch.rand(32, 200, generator=_gen(2), device="cuda")
+    big = torch.randn(8192, 8192, device="cuda")
+    w, b = torch.zeros_like(final), torch.zeros(120, device="cuda")
+    want = torch.empty(32, 120, device="cuda")
+    with _mx().Layer(cfg, None, final, b) as layer:
+        layer.forward(x, torch.empty_like(want), want)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(4):
+        big @ big                                       # (milliseconds of work before the weights are written)
+    w.copy_(final)
+    layer = _mx().Layer(cfg, None, w, b, stream=side)
+    got = torch.empty_like(want)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        layer.forward(x, torch.empty_like(want), got)
+    side.synchronize()
+    assert torch.equal(got, want)
+    layer.close()
