@@ -281,8 +281,8 @@ bcpnn_status bcpnn_profile_read_kernel(bcpnn_layer *layer, int32_t kernel, doubl
  * device, NULL = the null stream) and return without waiting, allocate nothing, keep nothing and can
  * be captured into a HIP graph.  The same call gives the same bits.  Matrices of numbers are
  * row-major with `ld` elements from row to row (ld >= columns; any alignment of their type).  A launch
- * stays below 2^32 work-items: a matrix of 2^24 pieces of 32 x 256 values, or a product that needs more, is
- * refused. */
+ * stays below 2^32 work-items: a matrix of 2^24 pieces of 32 x 256 values (by column, with its rows filled
+ * up to a multiple of 256), or a product that needs more, is refused. */
 typedef enum { BCPNN_F32 = 0, BCPNN_F16 = 1, BCPNN_BF16 = 2 } bcpnn_dtype;
 
 /* Bytes of an MX operand, -1 if the sizes are out of range. */

@@ -241,7 +241,8 @@ hipError_t launch_mx_quantize(hipStream_t stream, const void* src, int32_t dtype
                               int64_t ld, void* by_row, void* by_col);
 hipError_t launch_mx_dequantize(hipStream_t stream, const void* mx, int64_t rows, int64_t cols, void* dst,
                                 int32_t dtype, int64_t ld);
-int64_t mx_quantize_workgroups(int64_t rows, int64_t cols);   // of the larger launch
+// Workgroups of quantising (by_col: by column, or both ways) or, as by row, of reading back.
+int64_t mx_quantize_workgroups(int64_t rows, int64_t cols, bool by_col);
 
 // c = alpha a b^T + beta c + bias; work holds mx_product_work_bytes.
 hipError_t launch_mx_product(hipStream_t stream, const void* a, const void* b, int64_t m, int64_t n, int64_t k,

@@ -240,8 +240,8 @@ hipError_t launch_mx_dequantize(hipStream_t stream, const void* mx, int64_t rows
     }
 }
 
-int64_t mx_quantize_workgroups(int64_t rows, int64_t cols) {
-    return mx_groups(cols) * 8 * mx_groups(rows);
+int64_t mx_quantize_workgroups(int64_t rows, int64_t cols, bool by_col) {
+    return mx_groups(cols) * (by_col ? 8 * mx_groups(rows) : mx_row_blocks(rows));
 }
 
 }  // namespace bcpnn

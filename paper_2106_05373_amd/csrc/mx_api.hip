@@ -149,7 +149,7 @@ bcpnn_status bcpnn_mx_quantize(const void* src_dev, int32_t dtype, int64_t rows,
     if (!by_row_dev && !by_col_dev) return fail(BCPNN_EINVAL, "by_row_dev or by_col_dev is required");
     if (misaligned(by_row_dev) || misaligned(by_col_dev))
         return fail(BCPNN_EINVAL, "MX operands must be 16-byte aligned");
-    if (bcpnn::mx_quantize_workgroups(rows, cols) >= kMostWorkgroups)
+    if (bcpnn::mx_quantize_workgroups(rows, cols, by_col_dev != nullptr) >= kMostWorkgroups)
         return fail(BCPNN_EINVAL, "the matrix is too large for one launch");
     return launched(bcpnn::launch_mx_quantize((hipStream_t)hip_stream, src_dev, dtype, rows, cols, ld, by_row_dev,
                                               by_col_dev), "MX quantisation");
@@ -160,7 +160,7 @@ bcpnn_status bcpnn_mx_dequantize(const void* mx_dev, int64_t rows, int64_t cols,
     if (bcpnn_status st = check_matrix("dst_dev", dst_dev, dtype, rows, cols, ld)) return st;
     if (rows == 0 || cols == 0) return BCPNN_OK;
     if (!mx_dev || misaligned(mx_dev)) return fail(BCPNN_EINVAL, "mx_dev is required, 16-byte aligned");
-    if (bcpnn::mx_quantize_workgroups(rows, cols) >= kMostWorkgroups)
+    if (bcpnn::mx_quantize_workgroups(rows, cols, false) >= kMostWorkgroups)
         return fail(BCPNN_EINVAL, "the matrix is too large for one launch");
     return launched(bcpnn::launch_mx_dequantize((hipStream_t)hip_stream, mx_dev, rows, cols, dst_dev, dtype, ld),
                     "reading an MX operand");

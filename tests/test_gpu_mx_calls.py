@@ -160,3 +160,21 @@ def test_a_layer_on_another_stream_waits_for_its_weights():
     side.synchronize()
     assert torch.equal(got, want)
     layer.close()
+
+
+def test_one_long_row_is_quantised_by_row_and_read_back():
+    """2^21 pieces of 32 x 256: a launch of 2^29 work-items."""
+    import torch
+    mx = _mx()
+    cols = 1 << 29
+    x = torch.zeros(1, cols, device="cuda", dtype=torch.bfloat16)
+    ends = torch.cat([torch.arange(64), cols // 2 + torch.arange(64), cols - 64 + torch.arange(64)]).cuda()
+    x[0, ends] = torch.randn(192, generator=_gen(1), device="cuda").bfloat16()
+    m = mx.quantize(x)
+    out = mx.dequantize(m, torch.bfloat16)
+    want = mx_plain.quantized(x[:, ends].double().cpu().numpy())
+    assert np.array_equal(out[:, ends].double().cpu().numpy(), want)
+    out[0, ends] = 0
+    assert not bool(out.any())
+    with pytest.raises(_bcpnn().BcpnnError):            # 2^24 pieces with the rows filled up to 256
+        mx.quantize(x, rows=False, columns=True)
