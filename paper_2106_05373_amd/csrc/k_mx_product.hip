@@ -490,7 +490,8 @@ int64_t mx_product_work_items(int64_t m, int64_t n, int64_t k) {
     const Plan p = plan(m, n, k);
     const int64_t mb = mx_row_blocks(m), nb = mx_row_blocks(n);
     if (p.tile) return ((mb + p.tile - 1) / p.tile) * ((nb + p.tile - 1) / p.tile) * (p.tile == 8 ? 512 : 256);
-    return std::max(nb * ((mb + p.m_blocks - 1) / p.m_blocks) * p.splits * p.waves * 64, m * n);
+    const int64_t rows = nb * ((mb + p.m_blocks - 1) / p.m_blocks) * p.splits * p.waves * 64;
+    return p.splits > 1 ? std::max(rows, m * n) : rows;
 }
 
 int64_t mx_product_work_bytes(int64_t m, int64_t n, int64_t k) {

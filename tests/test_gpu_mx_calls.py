@@ -178,3 +178,19 @@ def test_one_long_row_is_quantised_by_row_and_read_back():
     assert not bool(out.any())
     with pytest.raises(_bcpnn().BcpnnError):            # 2^24 pieces with the rows filled up to 256
         mx.quantize(x, rows=False, columns=True)
+
+
+def test_product_of_few_rows_and_very_many_columns():
+    """2^32 outputs, of which a work-item stores several: a launch of 2^29."""
+    import torch
+    mx = _mx()
+    m, n = 64, 1 << 26
+    a = torch.randn(m, 1, generator=_gen(1), device="cuda")
+    b = torch.randn(n, 1, generator=_gen(2), device="cuda").half()
+    qa, qb = mx.quantize(a), mx.quantize(b)
+    del b
+    c = mx.product(qa, qb, dtype=torch.float16)
+    av, bv = mx.dequantize(qa), mx.dequantize(qb)
+    at = torch.cat([torch.arange(100), n // 2 + torch.arange(100), n - 100 + torch.arange(100)]).cuda()
+    want = av @ bv[at].t()                              # one product of 4-bit values: exact
+    assert torch.equal(c[:, at], want.half())
