@@ -20,8 +20,10 @@ from .bcpnn import _check, _dev_ptr, _host, lib
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 # Small calls are bound by the host (a launch takes 3 us of it), so the checks build no objects, and the
-# current stream comes as the number that it is (a torch.cuda.Stream of it costs 1.8 us).
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# current stream comes as the number that it is (a torch.cuda.Stream of it costs 1.8 us) where this torch
+# has it so.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                      lambda device: torch.cuda.current_stream(device).cuda_stream)
 _current_device = torch.cuda.current_device
 
 
