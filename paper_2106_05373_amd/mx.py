@@ -4,7 +4,7 @@ A Matrix is a matrix in blocks of 32 values along its rows, each with one power-
 4-bit code per value, in a device buffer as the matrix instructions read it.  quantize makes one,
 dequantize gives its values, product multiplies two; Layer is a BCPNN layer for inference on 4-bit
 weights.  The functions enqueue on PyTorch's current stream of the tensors' device and wait for
-nothing; a Layer enqueues on the stream it was made on.
+nothing; a Layer enqueues on the stream it was made on, whose device its tensors are on.
 """
 from __future__ import annotations
 
@@ -27,6 +27,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
 _current_device = torch.cuda.current_device
 
 
+_forward, _readout, _predict = lib.bcpnn_mx_forward, lib.bcpnn_mx_readout, lib.bcpnn_mx_predict
 _quantize, _dequantize, _product = lib.bcpnn_mx_quantize, lib.bcpnn_mx_dequantize, lib.bcpnn_mx_product
 _operand_bytes, _product_bytes = lib.bcpnn_mx_bytes, lib.bcpnn_mx_product_bytes
 
@@ -93,6 +94,21 @@ def _call(fn, device, *args):
     else:
         with torch.cuda.device(device):
             _check(fn(*args, _raw_stream(device)))
+
+
+def _ptr(t, name, dtype, shape, device):
+    """_dev_ptr of a tensor on a layer's device: its kernels run there, whichever device is current."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        raise (ValueError if getattr(t, "is_cuda", False) else TypeError)(f"{name} must be a tensor on cuda:{device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    return t.data_ptr()
 
 
 def quantize(x: torch.Tensor, rows: bool = True, columns: bool = False, out=None):
@@ -171,29 +187,33 @@ class Layer:
     def __init__(self, cfg: bcpnn.Config, mask: Optional[np.ndarray], w: torch.Tensor, b: torch.Tensor,
                  stream=None):
         n_in, n_out = cfg.in_hcu * cfg.in_mcu, cfg.out_hcu * cfg.out_mcu
-        current = torch.cuda.current_stream()
+        pw, pb = _dev_ptr(w, "w", torch.float32, (n_in, n_out)), _dev_ptr(b, "b", torch.float32, (n_out,))
+        current = torch.cuda.current_stream(None if w is None else w.device)
         stream = current if stream is None else stream
+        for t in (w, b):
+            if t is not None and t.get_device() != stream.device_index:
+                raise ValueError(f"w and b must be on the stream's device, cuda:{stream.device_index}")
         if stream.cuda_stream != current.cuda_stream:
             stream.wait_stream(current)
         keep = None if mask is None else _host(mask, np.uint8, (cfg.in_hcu, cfg.out_hcu))
         h = ctypes.c_void_p()
-        _check(lib.bcpnn_mx_create(ctypes.byref(cfg), None if keep is None else keep.ctypes.data,
-                                   _dev_ptr(w, "w", torch.float32, (n_in, n_out)),
-                                   _dev_ptr(b, "b", torch.float32, (n_out,)),
-                                   ctypes.c_void_p(stream.cuda_stream), ctypes.byref(h)))
+        with torch.cuda.device(stream.device_index):
+            _check(lib.bcpnn_mx_create(ctypes.byref(cfg), None if keep is None else keep.ctypes.data, pw, pb,
+                                       ctypes.c_void_p(stream.cuda_stream), ctypes.byref(h)))
         self._own(cfg, stream, h)
 
     @classmethod
     def of(cls, layer: bcpnn.Layer) -> "Layer":
         """The present weights, biases and mask of `layer`, on its stream."""
         h = ctypes.c_void_p()
-        _check(lib.bcpnn_mx_from_layer(layer._h, ctypes.byref(h)))
+        with torch.cuda.device(layer.stream.device_index):
+            _check(lib.bcpnn_mx_from_layer(layer._h, ctypes.byref(h)))
         self = cls.__new__(cls)
         self._own(layer.cfg, layer.stream, h)
         return self
 
     def _own(self, cfg, stream, h):
-        self.cfg, self.stream, self._h = cfg, stream, h
+        self.cfg, self.stream, self.device, self._h = cfg, stream, stream.device_index, h
         self.n_in, self.n_out = cfg.in_hcu * cfg.in_mcu, cfg.out_hcu * cfg.out_mcu
 
     def close(self):
@@ -215,21 +235,30 @@ class Layer:
 
     def forward(self, x, y, s=None):
         """y (and s, the support) [B][N_out] of x [B][N_in]."""
-        B = x.shape[0]
-        _check(lib.bcpnn_mx_forward(self._h, _dev_ptr(x, "x", torch.float32, (B, self.n_in)), B,
-                                    _dev_ptr(y, "y", torch.float32, (B, self.n_out)),
-                                    _dev_ptr(s, "s", torch.float32, (B, self.n_out))))
+        B, device = x.shape[0], self.device
+        if device != _current_device():
+            with torch.cuda.device(device):
+                return self.forward(x, y, s)
+        _check(_forward(self._h, _ptr(x, "x", torch.float32, (B, self.n_in), device), B,
+                        _ptr(y, "y", torch.float32, (B, self.n_out), device),
+                        _ptr(s, "s", torch.float32, (B, self.n_out), device)))
 
     def readout(self, x, winner):
         """winner [B][out_hcu]: the MCU of the largest support."""
-        B = x.shape[0]
-        _check(lib.bcpnn_mx_readout(self._h, _dev_ptr(x, "x", torch.float32, (B, self.n_in)), B,
-                                    _dev_ptr(winner, "winner", torch.int32, (B, self.cfg.out_hcu))))
+        B, device = x.shape[0], self.device
+        if device != _current_device():
+            with torch.cuda.device(device):
+                return self.readout(x, winner)
+        _check(_readout(self._h, _ptr(x, "x", torch.float32, (B, self.n_in), device), B,
+                        _ptr(winner, "winner", torch.int32, (B, self.cfg.out_hcu), device)))
 
     def predict_with(self, readout, x, y, winner):
         """winner [B]: the argmax of the 4-bit layer `readout` over this layer's activities of x
         [B][N_in], as many rows per launch as the workspace y [rows][N_out] has."""
-        B = x.shape[0]
-        _check(lib.bcpnn_mx_predict(self._h, readout._h, _dev_ptr(x, "x", torch.float32, (B, self.n_in)), B,
-                                    _dev_ptr(y, "y", torch.float32, (y.shape[0], self.n_out)), y.shape[0],
-                                    _dev_ptr(winner, "winner", torch.int32, (B,))))
+        B, rows, device = x.shape[0], y.shape[0], self.device
+        if device != _current_device():
+            with torch.cuda.device(device):
+                return self.predict_with(readout, x, y, winner)
+        _check(_predict(self._h, readout._h, _ptr(x, "x", torch.float32, (B, self.n_in), device), B,
+                        _ptr(y, "y", torch.float32, (rows, self.n_out), device), rows,
+                        _ptr(winner, "winner", torch.int32, (B,), device)))

@@ -125,9 +125,9 @@ class QuantizedNetwork:
         win = out
         if (out is None or not out.is_cuda or out.dtype != torch.int32 or out.shape != (B,)
                 or not out.is_contiguous()):
-            win = torch.empty(B, device="cuda", dtype=torch.int32)
+            win = torch.empty(B, device=self._rows.device, dtype=torch.int32)
         if B > 0:
-            stream, current = self.hidden.stream, torch.cuda.current_stream()
+            stream, current = self.hidden.stream, torch.cuda.current_stream(self._rows.device)
             other = stream.cuda_stream != current.cuda_stream
             if other:
                 stream.wait_stream(current)
