@@ -57,18 +57,20 @@ struct Tile {
     static_assert((kM + kN) % kWaves == 0, "whole row blocks per wave");
 };
 
-// Bound by the loads into LDS (29 bytes per cycle and CU at most) and the matrix instructions together,
-// each near its limit: 8192 x 8192 x 10000 takes 304 to 320 us (4.2 to 4.4 PFLOP/s; a loop of the
-// instruction alone reaches 6.6; with the loads but no LDS reads, or without the barriers, this kernel is
-// no faster).
+// Bound by the loads into LDS and the matrix instructions, which overlap in part only (below): 8192 x 8192 x
+// 10000 takes 312 us with bf16 results (4.3 PFLOP/s; a loop of the instruction alone reaches 6.6), 355 with
+// fp32.  With one tile per workgroup and bf16 results it took 329, without the loads 282, the matrix
+// instructions alone 260, the loads alone 202 (29 bytes per cycle and CU).
 // 2 x 4 waves of 4 x 2 blocks (128 accumulators a wave, two waves per SIMD) rather than 2 x 2 of 4 x 4:
 // those read a third less LDS, but spill around the loop (377 us against 458 when first measured).
 //
 // Both operands go through LDS in halves of a group, 128 columns (global_load_lds: 1 KiB of codes or
-// 256 bytes of scales per instruction, in the order the waves read them).  Four halves are held: one
-// being multiplied, three on their way, since a line that no neighbour has brought to the L2 takes
-// longer than the products of a whole group.  The halves are separate arrays, so that the reads of one
-// do not wait for the loads into the others.
+// 256 bytes of scales per instruction, in the order the waves read them).  Four halves are held, in
+// separate arrays, so that the reads of one do not wait for the loads into the others: one being
+// multiplied and up to three on their way.  That is so at one barrier in four: ahead of the other three,
+// of an odd last group's and of a tile's first the compiler waits for every load in flight
+// (s_waitcnt vmcnt(0) beside the fence of LDS in its listing), so that three half steps in four wait for the
+// loads that the one before requested.
 template <typename T, typename S>
 __global__ void __launch_bounds__(S::kThreads)
 product_tile_kernel(MxOperand a, MxOperand b, uint32_t m_tiles, uint32_t n_tiles, int64_t m_blocks,
@@ -165,8 +167,9 @@ product_tile_kernel(MxOperand a, MxOperand b, uint32_t m_tiles, uint32_t n_tiles
     };
     // One half (two steps), the first of which the wave has read.  The barrier stands between the steps:
     // by then every wave has read the whole half, so its place can be filled again (with the same half of
-    // the group after next), and the loads of the next half have arrived (those of the two after it may
-    // still be on their way), so its first step is read under the products of this one's second.
+    // the group after next), and the loads of the next half have arrived (those of the two after it need
+    // not have: kLater; the compiler's own wait leaves them in flight at place 0 only), so its first step is
+    // read under the products of this one's second.
     mx_codes ca[2][kTM], cb[2][kTN];
     uint32_t sa[2][kTM], sb[2][kTN];
     auto multiply = [&](auto place, int64_t g) __attribute__((always_inline)) {
@@ -197,15 +200,15 @@ product_tile_kernel(MxOperand a, MxOperand b, uint32_t m_tiles, uint32_t n_tiles
         request(p3, second);
     };
     // A workgroup takes a tile after another.  The next one's first halves are requested before this one's
-    // results are stored: the stores (7 us of a 256 x 256 tile's 80 when all CUs store at once) then pass under
-    // the next tile's products.
+    // results are turned around and stored (7 us of a 256 x 256 tile's 80 when all CUs store at once), and
+    // arrive under that.  The stores themselves do not pass under the next tile's products: store4 may read C,
+    // so that the compiler waits for all memory operations ahead of each of them, beta or not.
     int64_t mb, nb;
     blocks_of(blockIdx.x, mb, nb);
     if (kg > 0) {
         sources(mb, nb);
         request_first();
     }
-    bool stored = false;                                     // stores of known number follow the requests
     for (int64_t tile = blockIdx.x;;) {
 #pragma unroll
         for (int i = 0; i < kTM; ++i)
@@ -214,14 +217,7 @@ product_tile_kernel(MxOperand a, MxOperand b, uint32_t m_tiles, uint32_t n_tiles
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
         if (kg > 0) {
-            // The first halves are there.  The counter goes down in the order of issue: where only the stores
-            // came after these loads, half of them may be missing.
-            constexpr int kStores = kTM * 32 * kLanes / 64 / 2;
-            static_assert(kStores < 64, "fits the counter");
-            if (stored)
-                __builtin_amdgcn_s_waitcnt((kStores & 15) | ((kStores >> 4) << 14) | 0x0f70);
-            else
-                __builtin_amdgcn_s_waitcnt(0x0f70);
+            __builtin_amdgcn_s_waitcnt(0x0f70);              // vmcnt(0): the first halves are there
             lds_barrier();
             read(half0, 0, ca[0], cb[0]);
             read_scales(scales0, sa[0], sb[0]);
@@ -242,7 +238,6 @@ product_tile_kernel(MxOperand a, MxOperand b, uint32_t m_tiles, uint32_t n_tiles
         mx_quad bias;                                        // of the columns that this lane stores
 #pragma unroll
         for (int j = 0; j < 4; ++j) bias[j] = ep.bias_at(col + j);
-        stored = ep.beta == 0.0f && (mb + S::kM) * kMxRows <= ep.m && (nb + S::kN) * kMxRows <= ep.n;
         tile += gridDim.x;
         const bool more = tile < tiles;
         if (more) {
