@@ -194,3 +194,72 @@ def test_product_of_few_rows_and_very_many_columns():
     at = torch.cat([torch.arange(100), n // 2 + torch.arange(100), n - 100 + torch.arange(100)]).cuda()
     want = av @ bv[at].t()                              # one product of 4-bit values: exact
     assert torch.equal(c[:, at], want.half())
+
+
+# (sizes for each kind of tile, whole and not, several tiles per workgroup among them)
+TILES = [(900, 850, 700), (2304, 2560, 300), (2310, 2571, 700), (4352, 4096, 300), (4100, 4203, 700), (4100, 4203, 100)]
+HALF_STEP = {"float32": 2.0 ** -24, "float16": 2.0 ** -11, "bfloat16": 2.0 ** -8}
+
+
+@pytest.mark.parametrize("dtype", list(HALF_STEP))
+@pytest.mark.parametrize("m,n,k", TILES)
+def test_tiles_with_bias_scaling_accumulation_and_stride(m, n, k, dtype):
+    import torch
+    mx, g = _mx(), _gen(m + k)
+    T = getattr(torch, dtype)
+    a, b = (mx.quantize(torch.randn(r, k, generator=g, device="cuda")) for r in (m, n))
+    bias = torch.randn(n, generator=g, device="cuda")
+    av, bv = mx.dequantize(a).double(), mx.dequantize(b).double()
+    dot, mag = av @ bv.t(), av.abs() @ bv.abs().t()
+    for start, alpha, beta in ((0, 1.0, 0.0), (1, 0.375, -0.5), (3, -2.0, 1.0)):
+        room = torch.randn(m + 1, n + 5, generator=g, device="cuda").to(T)
+        before = room.clone()
+        out = room[:m, start:start + n]
+        c0 = out.double()
+        mx.product(a, b, bias=bias, alpha=alpha, beta=beta, out=out)
+        want = alpha * dot + beta * c0 + bias.double()
+        size = abs(alpha) * mag + (beta * c0).abs() + bias.double().abs()
+        # the sum's bound, then one rounding to the type of a value within it
+        bound = size * mx_plain.sum_bound(k) * (1 + HALF_STEP[dtype])
+        if dtype != "float32":
+            bound = bound + want.abs() * HALF_STEP[dtype] + (2.0 ** -25 if dtype == "float16" else 0.0)
+        assert bool(((out.double() - want).abs() <= bound).all()), (start, alpha, beta)
+        out.copy_(before[:m, start:start + n])
+        assert torch.equal(room, before)                # nothing beside the output changed
+
+
+@pytest.mark.parametrize("m,n,k", [(30, 500, 5000), (40, 256, 3000), (200, 300, 700), (900, 850, 260), (2304, 2560, 300),
+                                   (4100, 4203, 300)])
+def test_a_row_of_a_product_does_not_depend_on_the_other_rows(m, n, k):
+    import torch
+    mx, g = _mx(), _gen(m)
+    x, w = (torch.randn(r, k, generator=g, device="cuda") for r in (m, n))
+    b = mx.quantize(w)
+    c = mx.product(mx.quantize(x), b)
+    for row in (0, m // 2, m - 1):
+        other = torch.randn(m, k, generator=g, device="cuda") * 100
+        other[(row + 1) % m] = float("nan")
+        other[row] = x[row]
+        assert torch.equal(mx.product(mx.quantize(other), b)[row], c[row]), row
+
+
+def test_products_of_far_scales():
+    """Scales from 2^-126 to 2^125 on both sides, met by zeros and by scales that take them back."""
+    import torch
+    mx = _mx()
+    e = np.array([-120, -60, 0, 60, 120])
+    a = np.zeros((20, 320), np.float32)
+    b = np.zeros((20, 320), np.float32)
+    for i in range(5):
+        a[4 * i:4 * i + 4, 64 * i:64 * i + 32] = np.ldexp(1.5, e[i])       # meets the opposite scale: 2.25
+        b[4 * i:4 * i + 4, 64 * i:64 * i + 32] = np.ldexp(1.5, -e[i])
+        a[4 * i:4 * i + 4, 64 * i + 32] = np.ldexp(1.0, 120)               # meets a zero of a block as large
+        b[4 * i:4 * i + 4, 64 * i + 33] = np.ldexp(1.0, 120)
+    want, _ = mx_plain.product(mx_plain.quantized(a), mx_plain.quantized(b))
+    assert np.array_equal(want[::4, ::4], 72 * np.eye(5))
+    for rows in (1, 20, 900):
+        at = np.resize(np.arange(20), rows)
+        t = torch.from_numpy(a[at]).cuda()
+        u = torch.from_numpy(np.resize(b, (900 if rows == 900 else 20, 320))).cuda()
+        got = mx.product(mx.quantize(t), mx.quantize(u)).double().cpu().numpy()
+        assert np.array_equal(got[:, :20], want[at]), rows
