@@ -263,3 +263,52 @@ def test_products_of_far_scales():
         u = torch.from_numpy(np.resize(b, (900 if rows == 900 else 20, 320))).cuda()
         got = mx.product(mx.quantize(t), mx.quantize(u)).double().cpu().numpy()
         assert np.array_equal(got[:, :20], want[at]), rows
+
+
+def test_a_batch_transposed_in_pieces_against_the_definition():
+    """60000 inputs, of which 256 rows fit the transposition's workspace: rows of both pieces."""
+    import torch
+    B = _bcpnn()
+    g = np.random.default_rng(4)
+    hi, ho, mo, n = 30000, 100, 8, 300
+    mask = np.zeros((hi, ho), np.uint8)
+    for h in range(ho):
+        mask[g.choice(hi, 500 - 3 * h, replace=False), h] = 1
+    w = torch.randn(2 * hi, ho * mo, generator=_gen(1), device="cuda")
+    b = torch.randn(ho * mo, generator=_gen(2), device="cuda")
+    cfg = B.default_config(hi, 2, ho, mo, n, gain=2.0)
+    x = torch.rand(n, 2 * hi, generator=_gen(3), device="cuda")
+    room = torch.full((2, n + 2, ho * mo), 55.0, device="cuda")
+    y, s = room[0, :n], room[1, :n]
+    with _mx().Layer(cfg, mask, w, b) as layer:
+        layer.forward(x, y, s)
+    assert bool((room[:, n:] == 55.0).all())
+    rows = [0, 31, 32, 255, 256, 287, 288, 299]
+    yo, so, err = mx_plain.forward(cfg, mask, w.cpu().numpy(), b.cpu().numpy(), x[rows].cpu().numpy())
+    y, s = y[rows].double().cpu().numpy(), s[rows].double().cpu().numpy()
+    assert np.all(np.abs(s - so) <= err)
+    rel = np.repeat(mx_plain.softmax_bound(cfg, so, err), mo, 1)
+    assert np.all(np.abs(y - yo) <= rel * yo + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("storage", ["bf16", "m10"])
+@pytest.mark.parametrize("pairs", [0, 1])
+def test_layer_of_every_storage_format(storage, pairs):
+    import torch
+    B = _bcpnn()
+    cfg = B.default_config(64, 2, 4, 16, 32, alpha=0.05, seed=3, storage=storage, complement_pairs=pairs)
+    mask = np.zeros((64, 4), np.uint8)
+    for h in range(4):
+        mask[h:h + 20 + h, h] = 1
+    pixels = torch.rand(32, 64, generator=_gen(1), device="cuda")
+    x = torch.stack([pixels, 1 - pixels], 2).reshape(32, 128).contiguous()
+    y, s = (torch.empty(32, 64, device="cuda") for _ in range(2))
+    with B.Layer(cfg, mask) as trained:
+        for _ in range(3):
+            trained.train_batch(x)
+            trained.structural_update(count=False)
+        with _mx().Layer.of(trained) as layer:
+            layer.forward(x, y, s)
+        st = trained.get_state(("w", "b", "mask"))
+    _, so, err = mx_plain.forward(cfg, st["mask"], st["w"], st["b"], x.cpu().numpy())
+    assert np.all(np.abs(s.double().cpu().numpy() - so) <= err)
