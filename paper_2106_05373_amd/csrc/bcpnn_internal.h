@@ -276,7 +276,6 @@ hipError_t launch_mx_pack(hipStream_t stream, const Geometry& g, const float* w,
 hipError_t launch_mx_forward(hipStream_t stream, const Geometry& g, const float* x, int32_t B, const void* codes,
                              const void* scales, const float* bias, const ActiveUnits& act, float gain, float* turned,
                              int64_t turned_rows, float* y, float* s, int32_t* winner);
-int64_t mx_forward_turned_rows(const Geometry& g, int32_t max_batch);
 hipError_t mx_forward_prepare();     // before the first launch on a device
 
 // Makes a 4-bit layer from device arrays w [n_in][n_out], b and lists, on `stream`.  Waits.

@@ -114,9 +114,9 @@ forward_kernel(Geometry g, ForwardShape shape, const float* __restrict__ x, int3
     const int half = lane >> 5;
     // x as this workgroup's base, the same for all lanes, and 32-bit offsets in bytes: a lane's row
     // (past the last row: that one) and a unit
-    const char* base = reinterpret_cast<const char*>(kVec ? x + row0 * g.n_in : x + row0);
-    const uint32_t my_row = (uint32_t)min((int64_t)(lane & 31), B - 1 - row0) * 4u * (kVec ? (uint32_t)g.n_in : 1u);
-    const uint32_t unit_step = 4u * (kVec ? 1u : (uint32_t)stride);
+    const char* base = reinterpret_cast<const char*>(x + mx_input_base(kVec == 0, row0, g.n_in));
+    const InputSteps in = mx_input_steps(kVec == 0, g.n_in, stride);
+    const uint32_t my_row = mx_live_row(lane & 31, B - row0) * in.row;
     const int32_t* units = act.units + (int64_t)h * kg * kMxGroup;
 
     mx_acc acc[kTiles];
@@ -126,7 +126,7 @@ forward_kernel(Geometry g, ForwardShape shape, const float* __restrict__ x, int3
         for (int e = 0; e < 16; ++e) acc[t][e] = 0.0f;
     struct Weights { mx_codes c[4]; uint32_t s; };
     auto load_w = [&](Weights& w, int t, int grp) __attribute__((always_inline)) {
-        const int64_t at = ((int64_t)h * tiles + tile0 + t * n_waves) * kg + grp;
+        const int64_t at = mx_weight_group(h, tiles, (int64_t)tile0 + t * n_waves, kg, grp);
         w.s = scales[at * 64 + lane];
 #pragma unroll
         for (int st = 0; st < 4; ++st)
@@ -149,7 +149,7 @@ forward_kernel(Geometry g, ForwardShape shape, const float* __restrict__ x, int3
                 const int32_t* u = units + k0 + st * kMxStep;    // (the wave's: scalar loads)
 #pragma unroll
                 for (int i = 0; i < 32; i += kStep) {
-                    const uint32_t lo = (uint32_t)u[i] * unit_step, hi = (uint32_t)u[32 + i] * unit_step;
+                    const uint32_t lo = (uint32_t)u[i] * in.unit, hi = (uint32_t)u[32 + i] * in.unit;
                     const vec q = *reinterpret_cast<const vec*>(base + ((half ? hi : lo) + my_row));
 #pragma unroll
                     for (int e = 0; e < kStep; ++e) v[i + e] = q[e];
@@ -190,7 +190,7 @@ forward_kernel(Geometry g, ForwardShape shape, const float* __restrict__ x, int3
 
     // supports to LDS, each part's sums in a place of their own (the first with the bias)
     float* sup = reinterpret_cast<float*>(lds);
-    const int pitch = mx_support_pitch(M), place = kMxRows * pitch;
+    const int pitch = mx_support_pitch(M);
     __syncthreads();
     if (works) {
 #pragma unroll
@@ -199,7 +199,7 @@ forward_kernel(Geometry g, ForwardShape shape, const float* __restrict__ x, int3
             if (c >= M) continue;
             const float b = part == 0 ? bias[(int64_t)h * M + c] : 0.0f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sup[part * place + mx_row(e, half) * pitch + c] = acc[t][e] + b;
+            for (int e = 0; e < 16; ++e) sup[mx_support_at(part, mx_row(e, half), pitch, c)] = acc[t][e] + b;
         }
     }
     __syncthreads();
@@ -208,14 +208,14 @@ forward_kernel(Geometry g, ForwardShape shape, const float* __restrict__ x, int3
         const int64_t row = row0 + r;
         if (row >= B) continue;                              // uniform over the 16 lanes
         const int l = tid & 15;
-        float* d = sup + r * pitch;
+        float* d = sup + mx_support_at(0, r, pitch, 0);
         const int64_t o = row * g.n_out + (int64_t)h * M;
         float top = -INFINITY;                               // (a NaN takes no part)
         int at = 0x7fffffff;
         for (int c = 4 * l; c < M; c += 64) {
             mx_quad v = *reinterpret_cast<mx_quad*>(d + c);
             if (parts > 1) {
-                for (int p = 1; p < parts; ++p) v += *reinterpret_cast<mx_quad*>(d + p * place + c);
+                for (int p = 1; p < parts; ++p) v += *reinterpret_cast<mx_quad*>(sup + mx_support_at(p, r, pitch, c));
                 *reinterpret_cast<mx_quad*>(d + c) = v;
             }
 #pragma unroll
@@ -275,9 +275,7 @@ forward_rows_kernel(Geometry g, const float* __restrict__ x, int32_t B, const ui
         }
     }
     __syncthreads();
-    const float* mine = xs + min(c0, rows - 1) * pitch;
-    // this lane's block of 16 columns and 128 units, in the operand of 32 rows and steps of 64
-    const int wl = 32 * (quarter & 1) + c0;
+    const float* mine = xs + (int)mx_live_row(c0, rows) * pitch;
     for (int h = wave; h < g.out_hcu; h += kMxWaves) {
         const int k_total = act.count[h], kg = act.kg;
         const int32_t* units = act.units + (int64_t)h * kg * kMxGroup;
@@ -285,13 +283,13 @@ forward_rows_kernel(Geometry g, const float* __restrict__ x, int32_t B, const ui
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) acc[t] = mx_acc16{0.0f, 0.0f, 0.0f, 0.0f};
         for (int k0 = 0; k0 < k_total; k0 += 128) {
-            const int step = k0 / kMxStep % 4 + quarter / 2;
+            const int step = mx_rows_step(k0, quarter);
             mx_codes w[kTiles];
             uint32_t ws[kTiles];
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
-                const int64_t at = ((int64_t)h * rbs + min(t / 2, rbs - 1)) * kg + k0 / kMxGroup;
-                const int l = wl + 16 * (t & 1);
+                const int64_t at = mx_weight_group(h, rbs, mx_rows_block(t, rbs), kg, k0 / kMxGroup);
+                const int l = mx_rows_lane(c0, quarter, t);
                 w[t] = reinterpret_cast<const mx_codes*>(codes + at * kMxGroupCodes)[64 * step + l];
                 ws[t] = scales[at * 64 + l] >> (8 * step);
             }
@@ -416,12 +414,6 @@ hipError_t mx_forward_prepare() {
                 e = hipFuncSetAttribute((const void*)forward_for(tiles, vec),
                                         hipFuncAttributeMaxDynamicSharedMemorySize, kMxForwardLds);
     return e;
-}
-
-// Rows of the transposed input: as many as a batch has, within 64 MiB.
-int64_t mx_forward_turned_rows(const Geometry& g, int32_t max_batch) {
-    const int64_t fit = (64ll << 20) / 4 / g.n_in / 64 * 64;
-    return std::min<int64_t>(fit, ((int64_t)max_batch + 63) / 64 * 64);
 }
 
 namespace {

@@ -8,6 +8,7 @@
 
 #include "bcpnn_internal.h"
 #include "mx_format.h"
+#include "mx_layer_layout.h"
 
 using bcpnn::ActiveLists;
 using bcpnn::ActiveUnits;

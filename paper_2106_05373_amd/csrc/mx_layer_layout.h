@@ -71,6 +71,43 @@ inline bool mx_rows_in_lds(const Geometry& g, int64_t rows) {
            g.out_hcu >= kMxWaves && rows >= 200 * kMxTileRows;
 }
 
+// ---- Indices of the forward kernels, which the host's check follows ----
+
+// Where the inputs of a workgroup's first row begin (in floats), and the bytes from row to row and from unit
+// to unit: 32-bit offsets from there, x [rows][n_in] or, transposed, [n_in][stride].
+struct InputSteps { uint32_t row, unit; };
+__host__ __device__ inline int64_t mx_input_base(bool turned, int64_t row0, int64_t n_in) {
+    return turned ? row0 : row0 * n_in;
+}
+__host__ __device__ inline InputSteps mx_input_steps(bool turned, int64_t n_in, int32_t stride) {
+    return turned ? InputSteps{4u, 4u * (uint32_t)stride} : InputSteps{4u * (uint32_t)n_in, 4u};
+}
+// The row that a lane reads: its own, or the last of the rows that there are.
+__host__ __device__ inline uint32_t mx_live_row(int row, int64_t rows_left) {
+    return (uint32_t)(row < rows_left ? row : rows_left - 1);
+}
+// Group of the packed weights: `tiles` row blocks of kg groups for each hidden HCU.
+__host__ __device__ inline int64_t mx_weight_group(int h, int tiles, int64_t tile, int kg, int grp) {
+    return ((int64_t)h * tiles + tile) * kg + grp;
+}
+// Support of a row and a column in LDS, each part's in a place of its own.
+__host__ __device__ inline int mx_support_at(int part, int row, int pitch, int c) {
+    return part * (kMxRows * pitch) + row * pitch + c;
+}
+// Of forward_rows_kernel, whose lane takes a block of 16 rows or columns and 32 of 128 units (a quarter of
+// the wave each): row block, step of the group at k0 and lane of the weights of column tile t.
+__host__ __device__ inline int mx_rows_block(int t, int row_blocks) {
+    return t / 2 < row_blocks ? t / 2 : row_blocks - 1;
+}
+__host__ __device__ inline int mx_rows_step(int k0, int quarter) { return k0 / kMxStep % 4 + quarter / 2; }
+__host__ __device__ inline int mx_rows_lane(int c0, int quarter, int t) { return 32 * (quarter & 1) + c0 + 16 * (t & 1); }
+
+// Rows of the transposed input: as many as a batch has, within 64 MiB.
+inline int64_t mx_forward_turned_rows(const Geometry& g, int32_t max_batch) {
+    const int64_t fit = (64ll << 20) / 4 / g.n_in / 64 * 64;
+    return std::min<int64_t>(fit, ((int64_t)max_batch + 63) / 64 * 64);
+}
+
 // Codes and scales of a chunk; afterwards the parts' supports.
 inline size_t mx_forward_lds(const ForwardShape& f, int out_mcu) {
     const size_t chunk = (size_t)f.steps * (kMxStepCodes + kMxStep);

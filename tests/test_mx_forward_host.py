@@ -1,4 +1,4 @@
-"""The 4-bit layer's forward launches over the sizes a layer can have, on the host."""
+"""The launches and accesses of the 4-bit layer's forward pass over the sizes a layer can have, on the host."""
 import os
 import shutil
 import subprocess
@@ -11,7 +11,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 @pytest.mark.skipif(not os.path.exists(HIPCC) and shutil.which("hipcc") is None,
                     reason="hipcc is not available")
-def test_every_launch_fits(tmp_path):
+def test_every_launch_and_every_access_fits(tmp_path):
     exe = str(tmp_path / "mx_forward_check")
     cmd = [HIPCC, "--offload-arch=gfx950", "-O2", "-std=c++17", "-I", os.path.join(ROOT, "include"),
            "-I", os.path.join(ROOT, "paper_2106_05373_amd", "csrc"),
