@@ -20,12 +20,11 @@ from .bcpnn import _check, _dev_ptr, _host, lib
 DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 # Small calls are bound by the host (a launch takes 3 us of it), so the checks build no objects, and the
-# current stream comes as the number that it is (a torch.cuda.Stream of it costs 1.8 us) where this torch
-# has it so.
+# current stream and device come as the numbers that they are (a torch.cuda.Stream costs 1.8 us) where this
+# torch has them so.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                       lambda device: torch.cuda.current_stream(device).cuda_stream)
-_current_device = torch.cuda.current_device
-
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 _forward, _readout, _predict = lib.bcpnn_mx_forward, lib.bcpnn_mx_readout, lib.bcpnn_mx_predict
 _quantize, _dequantize, _product = lib.bcpnn_mx_quantize, lib.bcpnn_mx_dequantize, lib.bcpnn_mx_product
