@@ -7,8 +7,9 @@
 // the bound is the gather, since every (row, hidden HCU) pair reads inputs of its own, and in fp32, a
 // block's scale depending on its values.  Three forms, by what the gather costs (transposes,
 // mx_rows_in_lds): directly, a line per lane and load; from the transposed inputs, whole lines; from
-// LDS.  MNIST shape: 1 row 5.5 us, 512 rows 12, 8192 rows 68 (196 MB of stores); STL shape: 1 row 12.5,
-// 256 rows 72 (283 MB of gathered inputs and 141 MB of weights from L2).
+// LDS.  Four batches in turn, activities and supports: MNIST shape, 1 row 6.0 us, 128 rows 8.8, 8192 rows 78
+// (196 MB of stores; 64 where the same batch comes again, partly from the caches); STL shape, 1 row 12.8, 256
+// rows 82 (283 MB of gathered inputs and 141 MB of weights from L2; 71).
 #include <algorithm>
 
 #include "bcpnn_internal.h"

@@ -64,8 +64,9 @@ constexpr int kMxRowsLds = 150 * 1024;
 // Floats of such a row: whole quads, and rows lie 4 banks apart.
 __host__ __device__ inline int64_t mx_input_pitch(int64_t n_in) { return n_in + ((4 - n_in) & 63); }
 // Whether a launch takes it: the rows fit, one wave's tiles cover a hidden HCU, and row tiles and hidden
-// HCUs fill most of the chip.  Measured (us, this form / the other): MNIST shape, 8192 rows 70.6 / 105, 4096
-// rows 36.6 / 53, 2048 rows 36 / 32.9; 500 x 3 -> 17 x 70 units, 4096 rows 33.6 / 50.
+// HCUs fill most of the chip.  Measured (us, this form / the other): MNIST shape, 8192 rows 67 / 101, 4096
+// rows 34 / 50, 2048 rows 36 / 32.9; 500 x 3 -> 17 x 70 units, 4096 rows 33.6 / 50; 784 x 2 -> 30 HCUs of 2, 16
+// and 128 units, 3200 rows 19.5 / 34.8, 20.9 / 33.7 and 32.4 / 44.8; 40 x 4 -> 100 x 2, 3200 rows 38 / 51.
 inline bool mx_rows_in_lds(const Geometry& g, int64_t rows) {
     return kMxTileRows * mx_input_pitch(g.n_in) * 4 <= kMxRowsLds && mx_row_blocks(g.out_mcu) <= 4 &&
            g.out_hcu >= kMxWaves && rows >= 200 * kMxTileRows;
